@@ -284,9 +284,12 @@ int hisparse_read_records(const hisparse_record_format_t *format, int device, co
  * outside the tensors: a request whose rows leave q is skipped, a chunk longer than max_q_len is cut to it, a context
  * longer than max_kv_len or table_width pages ends there, a table entry beyond num_records is an absent page.
  * Arithmetic: products of the numbers as they are (quantised records as bf16, exactly for scales that are powers of two, or
- * as codes with their scales) summed in fp32 on the tensor cores, softmax in fp32, its weights rounded to bf16 or kept to 12
- * bits before they multiply the values, out rounded once to bf16: within 2^-7 * max |value| of the exact result, besides what
- * fp32 scores are off.  The same call gives the same bits every time.
+ * as codes with their scales) summed in fp32 on the tensor cores, softmax in fp32, its weights rounded to bf16, or to f16 next
+ * to codes, before they multiply the values, out rounded once to bf16: within 2^-7 * max |value| of the exact result, the
+ * values being those of the keys that the token attends: records of zeros, or of another size with a weight near zero, cost
+ * the others nothing.  (Next to codes a number is off by 2^-8 of itself, by 2^-11 of sum_j p_j |v_j| and by at most 2^-8 of
+ * the largest p_j |v_j| of its group of 128.)  Not counted is what fp32 scores are off.  The same call gives the same bits
+ * every time.
  * A record's scales are taken to be finite, not negative and powers of two, as hisparse_write_records leaves them; others are
  * read too, but may be rounded to bf16 with the code that they multiply.
  */

@@ -7,18 +7,23 @@
 //            exactly down to 2^-13 of the largest; below that they are off by at most 2^-22 of it.  S_g = codes_g t1^T,
 //            codes_g t2^T by group of 128 numbers, because the scales are by record and group:
 //            s = 2^a sum_g scale_g (S_g1 + S_g2 / 32) + tail, the bf16 tail in a product of its own.
-//   weights  p scale_g / 2^E_g = w1 + w2 / 32 + w3 / 1024, E_g the group's largest exponent so far: three terms are 12 bits
-//            (bf16 weights are 8), and what is too small for them is off by 2^-20.  The largest weight is kept between
-//            2^lift and 2^8, with lift such that all keys together are then off by at most 2^-8 of it, which is less than
-//            bf16's rounding: 0 for 2048 keys, 6 for 131072, the most that this kernel is given.  (A small lift leaves the
-//            running maximum room: it moves for a fraction of the tiles.  With 7 throughout, 32 x 32768 keys took 186 us
-//            instead of 157.)  O_g += codes_g w^T, out = 2^E_g (O_g1 + O_g2 / 32 + O_g3 / 1024).
+//   weights  p scale_g / 2^k = w1 + w2 / 32 + w3 / 1024, k by row and group: p is rounded to f16 (11 bits; bf16 weights are 8),
+//            which three terms hold, and what is too small for them is off by 2^-20.  What k follows is the largest p scale_g
+//            so far, the weight and the size of one and the same record, which comes to lie above 2^lift and at most at 2^8, with
+//            lift such that all keys together are off by at most 2^-8 of the largest p max |value| of the group, no more than
+//            bf16's rounding: 0 for 2048 keys, 6 for 131072, the most that this kernel is given.  A small lift leaves the
+//            maximum room, so that it moves for a fraction of the tiles (8 of 64; 32 x 32768 keys take 157 us with a lift of 4,
+//            150 with 3, 141 with 0).  A group of zeros has scale 1 and no size: it does not count, for which the codes of
+//            groups with that scale are looked at.  (With the largest scale in place of the largest p scale, 142 us, a record of
+//            zeros, or a large one that is not attended, took the weights of all others below the terms' reach.)  The running
+//            maximum of a row is a whole number, so that k moves with it exactly.
+//            O_g += codes_g w^T, out = 2^k (O_g1 + O_g2 / 32 + O_g3 / 1024).
 // Splits of a context meet in a cluster where there are 2, 4 or 8: every block leaves its O, m and l in shared memory and merges
 // a share of the numbers out of all of them, which saves the second kernel and its 2 x 33 KB a block through memory.
 // Both products are transposed as there: 128 keys or 128 numbers are M, R query rows times their terms are N.
-// 32 requests x 32768 keys of 656 bytes, 16 heads: 142 us, 4.7 TB/s, bound by the TMA's rows (each 128 bytes of such a record
-// lie in two lines; loads alone take 129 us); with stages released as a whole instead of by group 156 us.  32 x 2048 keys
-// through a slot table: 21.8 us, where four-row gathers (25 cycles
+// 32 requests x 32768 keys of 656 bytes, 16 heads: 157 us, 4.3 TB/s, bound by the TMA's rows (each 128 bytes of such a record
+// lie in two lines; loads alone take 129 us) and by the tiles whose maxima move; with stages released as a whole instead of by
+// group 14 us more.  32 x 2048 keys through a slot table: 22.5 us, where four-row gathers (25 cycles
 // each) and a block's start and end count as much as its four tiles.
 //   tile     128 keys: [group][key][128 bytes] of codes (K-major for S^T, MN-major for O^T) and [key][128 bytes] of tail, by TMA
 //            boxes or four-row gathers; two stages
@@ -37,6 +42,8 @@ constexpr int kDaTermsQ = 2, kDaTermsP = 3;
 
 template <int R>
 struct DaSmem {
+  static constexpr int kVG = R == 16 ? 4 : R == 32 ? 2 : 1;   // groups of values that tensor memory has room for beside R rows
+  static constexpr int kRed = R / 2 * (1 + kVG);              // numbers that a softmax warp reduces: its rows, then [row][group]
   // stages, query codes [group][2 R][128], query tail [R][128], weights [group][term][R / 16][key][16]
   __host__ __device__ static constexpr uint32_t stage(const int cg, const int tail) { return (uint32_t)((cg + tail) * kDaChunk); }
   __host__ __device__ static constexpr uint32_t q(const int cg, const int tail) { return 2 * stage(cg, tail); }
@@ -46,10 +53,11 @@ struct DaSmem {
   static constexpr int kBars = 2 + 2 * 4 + 2 + 2 + 1 + 2;
   __host__ __device__ static constexpr uint32_t tmem(const int cg, const int tail, const int vg) { return bars(cg, tail, vg) + 8 * (kBars + 1); }
   __host__ __device__ static constexpr uint32_t red(const int cg, const int tail, const int vg) { return (tmem(cg, tail, vg) + 31) / 16 * 16; }
-  __host__ __device__ static constexpr uint32_t fac(const int cg, const int tail, const int vg) { return red(cg, tail, vg) + kDaSoftWarps * (R / 2 + 4) * 4; }   // (a multiple of 16)
-  __host__ __device__ static constexpr uint32_t qs(const int cg, const int tail, const int vg) { return fac(cg, tail, vg) + R * 4; }
+  __host__ __device__ static constexpr uint32_t fac(const int cg, const int tail, const int vg) { return red(cg, tail, vg) + kDaSoftWarps * kRed * 4; }   // (a multiple of 16)
+  __host__ __device__ static constexpr uint32_t qs(const int cg, const int tail, const int vg) { return fac(cg, tail, vg) + R * kVG * 4; }
   __host__ __device__ static constexpr uint32_t max(const int cg, const int tail, const int vg) { return qs(cg, tail, vg) + R * 4; }
-  __host__ __device__ static constexpr uint32_t total(const int cg, const int tail, const int vg) { return max(cg, tail, vg) + R * 4; }
+  __host__ __device__ static constexpr uint32_t inv(const int cg, const int tail, const int vg) { return max(cg, tail, vg) + R * 4; }
+  __host__ __device__ static constexpr uint32_t total(const int cg, const int tail, const int vg) { return inv(cg, tail, vg) + R * kVG * 4; }
 };
 
 __host__ __device__ constexpr int da_cols(const int R, const int cg, const int tail, const int vg) {   // tensor-memory columns
@@ -70,6 +78,7 @@ constexpr uint32_t kDaPDescHi = 2048u >> 4 | 1u << 14;
 
 constexpr float kDaStep = 32.f;                  // from one term to the next
 constexpr int kDaMaxKeys = 1 << 17;
+constexpr int kDaLeast = -120;                   // smallest k: 2^-k times a scale and a weight stays a number
 
 // The codes of a pair of f16 numbers, and kDaStep times what they leave (exact: both are multiples of the number's last bit)
 __device__ __forceinline__ uint32_t e4m3_term(__half2 &x) {
@@ -80,10 +89,27 @@ __device__ __forceinline__ uint32_t e4m3_term(__half2 &x) {
   return c;
 }
 
+// 2^e of a whole number, 0 below 2^-126
+__device__ __forceinline__ float pow2_whole(const float e) {
+  return __int_as_float((min(max(__float2int_rn(e), -127), 127) + 127) << 23);
+}
 __device__ __forceinline__ float warp_max(const float v) {   // (a NaN is ignored)
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
+}
+// Lane i's v[0] becomes the largest v[i] of the warp's lanes: every step hands over half of the numbers that are left.
+__device__ __forceinline__ void warp_max_each(float (&v)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = 16; n; n >>= 1) {
+    const bool up = lane & n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float away = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + n], n);
+      v[i] = fmaxf(up ? v[i + n] : v[i], away);
+    }
+  }
 }
 // 32 lanes x 8 columns
 __device__ __forceinline__ void tmem_ld8(const uint32_t addr, float *v) {
@@ -164,11 +190,12 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
   const uint32_t sbase = smem_u32(ra_smem), s_q = sbase + L::q(cg, tail), s_qt = sbase + L::qt(cg, tail), s_p = sbase + L::p(cg, tail);
   const uint32_t stage_bytes = L::stage(cg, tail);
   const uint32_t b_full = sbase + L::bars(cg, tail, vg), b_empty = b_full + 16, b_s = b_empty + 64, b_p = b_s + 16, b_q = b_p + 16, b_end = b_q + 8;
-  float *s_red = reinterpret_cast<float *>(ra_smem + L::red(cg, tail, vg));   // [warp][R / 2 + 4]: rows, then groups
-  float *s_fac = reinterpret_cast<float *>(ra_smem + L::fac(cg, tail, vg));   // [row]
+  float *s_red = reinterpret_cast<float *>(ra_smem + L::red(cg, tail, vg));   // [warp][kRed]
+  float *s_fac = reinterpret_cast<float *>(ra_smem + L::fac(cg, tail, vg));   // [row][group], at the end [row]
   float *s_qs = reinterpret_cast<float *>(ra_smem + L::qs(cg, tail, vg));     // [row] 2^a times the scale, in the base-2 domain
 
-  float *s_max = reinterpret_cast<float *>(ra_smem + L::max(cg, tail, vg));   // [row] `lift` below the largest score, base 2
+  float *s_max = reinterpret_cast<float *>(ra_smem + L::max(cg, tail, vg));   // [row] running maximum of the scores, base 2, a whole number
+  float *s_inv = reinterpret_cast<float *>(ra_smem + L::inv(cg, tail, vg));   // [row][group] 2^-k
 
   const uint32_t item = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x - item * a.splits;
   const int n = (int)(item / (uint32_t)a.row_tiles), rt = (int)(item - (uint32_t)n * a.row_tiles);
@@ -323,7 +350,7 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax
-    constexpr int RH = R / 2, W = RH + 4;
+    constexpr int RH = R / 2, VG = L::kVG, W = L::kRed;
     const int key = tid & 127, part = tid >> 7, r0 = part * RH;   // this thread's key and rows
     // the records' scales, a tile ahead
     bool ignore = false;
@@ -389,6 +416,7 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
     }
     }
     if (tid < R) s_max[tid] = kRaLowest;
+    if (tid < R * VG) s_inv[tid] = pow2_whole((float)-kDaLeast);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(b_q);
@@ -398,7 +426,6 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float *red = s_red + part * 4 * W;      // of this part's four warps
     float l[RH];
-    float top_scale[4] = {0.f, 0.f, 0.f, 0.f}, inv_scale[4] = {0.f, 0.f, 0.f, 0.f};   // 2^E_g, 2^-E_g; 0 while no key has come
 #pragma unroll
     for (int r = 0; r < RH; ++r) l[r] = 0.f;
     for (int t = 0; t < nt; ++t) {
@@ -436,101 +463,136 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[h + i] = here ? acc[i] * qs[i] + (tail ? s3[i] * a.scale_log2e : 0.f) : -INFINITY;
       }
-      // scores above the running maximum (which lies `lift` below the largest so far: weights are at most 2^8)
-      bool raise = false;
+      // the scales that the weights are measured with: none where the group is zeros
+      float se[VG];
 #pragma unroll
-      for (int r = 0; r < RH; r += 4) {
-        const float4 m = *reinterpret_cast<const float4 *>(s_max + r0 + r);
-        raise |= fmaxf(fmaxf(x[r] - m.x, x[r + 1] - m.y), fmaxf(x[r + 2] - m.z, x[r + 3] - m.w)) > 8.f;
+      for (int g = 0; g < VG; ++g) {
+        se[g] = here && g < vg ? sg[g] : 0.f;
+        if (se[g] == 1.f) {
+          wait(b_full + 8 * st, (uint32_t)((t / 2) & 1));   // (it has come; the wait makes the codes visible to this thread)
+          const unsigned char *row = ra_smem + (uint32_t)st * stage_bytes + g * kDaChunk + key * 128;
+          uint32_t some = 0;
+#pragma unroll 1
+          for (int u = 0; u < 8 && !some; ++u) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(row + ((u ^ (key & 7)) << 4));
+            some = (v.x | v.y | v.z | v.w) & 0x7f7f7f7fu;
+          }
+          if (!some) se[g] = 0.f;
+        }
       }
+      // weights against the running maxima, and whether one is above 2^8
+      float p[RH], w[RH * VG];
+      auto weigh = [&] {
+        bool over = false;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) raise |= here && g < vg && sg[g] > top_scale[g];
-      if (softmax_any<kDaSoft>(raise)) {
+        for (int r = 0; r < RH; r += 4) {
+          const float4 m = *reinterpret_cast<const float4 *>(s_max + r0 + r);
+          p[r] = ex2(x[r] - m.x); p[r + 1] = ex2(x[r + 1] - m.y); p[r + 2] = ex2(x[r + 2] - m.z); p[r + 3] = ex2(x[r + 3] - m.w);
+          over |= fmaxf(fmaxf(p[r], p[r + 1]), fmaxf(p[r + 2], p[r + 3])) > 256.f;
+        }
+#pragma unroll
+        for (int i = 0; i < RH * VG; i += 4) {
+          const float4 inv = *reinterpret_cast<const float4 *>(s_inv + r0 * VG + i);
+          // (in this order no product is out of range before it is known to be above 2^8)
+          w[i] = p[i / VG] * se[i % VG] * inv.x;
+          w[i + 1] = p[(i + 1) / VG] * se[(i + 1) % VG] * inv.y;
+          w[i + 2] = p[(i + 2) / VG] * se[(i + 2) % VG] * inv.z;
+          w[i + 3] = p[(i + 3) / VG] * se[(i + 3) % VG] * inv.w;
+          over |= fmaxf(fmaxf(w[i], w[i + 1]), fmaxf(w[i + 2], w[i + 3])) > 256.f;
+        }
+        return over;
+      };
+      if (softmax_any<kDaSoft>(weigh())) {
 #pragma unroll
         for (int r = 0; r < RH; ++r) {
           const float v = warp_max(x[r]);
           if (lane == 0) s_red[warp * W + r] = v;
         }
+        float y[32];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float v = warp_max(here && g < vg ? sg[g] : 0.f);
-          if (lane == 0) s_red[warp * W + RH + g] = v;
+        for (int i = 0; i < 32; ++i) {
+          const float sc2 = i < RH * VG ? se[i % VG] : 0.f;
+          // (the exponent of the power of two at or above the scale)
+          y[i] = sc2 > 0.f ? x[i / VG < RH ? i / VG : 0] + (float)((int)((__float_as_uint(sc2) + 0x7fffffu) >> 23) - 127) : -INFINITY;
+        }
+        warp_max_each(y);
+        if (lane < RH * VG) s_red[warp * W + RH + lane] = y[0];
+        float before[RH];
+#pragma unroll
+        for (int r = 0; r < RH; r += 4) *reinterpret_cast<float4 *>(before + r) = *reinterpret_cast<const float4 *>(s_max + r0 + r);
+        softmax_sync<kDaSoft>();
+        const int mr = key / VG;                   // a thread a row and group
+        float mn = 0.f, inv = 0.f;
+        if (key < RH * VG) {
+          const float *v4 = red + mr, *y4 = red + RH + key;
+          const float v = fmaxf(fmaxf(v4[0], v4[W]), fmaxf(v4[2 * W], v4[3 * W])), top = fmaxf(fmaxf(y4[0], y4[W]), fmaxf(y4[2 * W], y4[3 * W]));
+          mn = fmaxf(s_max[r0 + mr], ceilf(v));
+          // k such that the largest weight so far lies between 2^lift and 2^(lift + 1)
+          const float drop = s_max[r0 + mr] - mn, k0 = (float)(127 - (int)(__float_as_uint(s_inv[r0 * VG + key]) >> 23));
+          const float k = fminf(fmaxf(ceilf(fmaxf(top - mn, k0 + lift + 1.f + drop)) - (lift + 1.f), (float)kDaLeast), 126.f);
+          inv = pow2_whole(-k);
+          s_fac[r0 * VG + key] = pow2_whole(drop + k0 - k);
         }
         softmax_sync<kDaSoft>();
-        float grow[4];                            // 2^(E_g before - E_g now)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float v = fmaxf(fmaxf(red[RH + g], red[W + RH + g]), fmaxf(red[2 * W + RH + g], red[3 * W + RH + g]));
-          grow[g] = 1.f;
-          if (v > top_scale[g]) {
-            // the power of two at or above it, 2^-126 to 2^126, and its reciprocal
-            const uint32_t up = max(min((__float_as_uint(v) + 0x7fffffu) & 0x7f800000u, 0x7e800000u), 0x00800000u);
-            inv_scale[g] = __uint_as_float(0x7f000000u - up);
-            grow[g] = top_scale[g] * inv_scale[g];
-            top_scale[g] = __uint_as_float(up);
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < RH; ++r) {
-          const float v = fmaxf(fmaxf(red[r], red[W + r]), fmaxf(red[2 * W + r], red[3 * W + r]));
-          const float m = s_max[r0 + r], al = ex2(m - fmaxf(m, v - lift));
-          l[r] *= al;
-          if (key == 0) s_fac[r0 + r] = al;
-        }
-        softmax_sync<kDaSoft>();
-        if (key < RH) {
-          const float v = fmaxf(fmaxf(red[key], red[W + key]), fmaxf(red[2 * W + key], red[3 * W + key]));
-          s_max[r0 + key] = fmaxf(s_max[r0 + key], v - lift);
+        if (key < RH * VG) {
+          s_inv[r0 * VG + key] = inv;
+          if (key % VG == 0) s_max[r0 + mr] = mn;
         }
         if (t > 0) {
           wait(b_empty + 8 * (4 * ((t - 1) & 1) + vg - 1), (uint32_t)(((t - 1) / 2) & 1));
           tmem_fence_after();
 #pragma unroll 1
           for (int g = 0; g < vg; ++g) {
-            const float gr = g == 0 ? grow[0] : g == 1 ? grow[1] : g == 2 ? grow[2] : grow[3];
 #pragma unroll 1
-            for (int k = 0; k < kDaTermsP; ++k)
-#pragma unroll 1
-              for (int h = 0; h < RH; h += 8) {
-                float o[8];
-                const uint32_t at = t_o + lanes + (uint32_t)((g * kDaTermsP + k) * R + r0 + h);
-                tmem_ld8(at, o);
-                tmem_wait_ld();
+            for (int h = 0; h < RH; h += 8) {
+              float o[kDaTermsP][8];
+              const uint32_t at = t_o + lanes + (uint32_t)(g * kDaTermsP * R + r0 + h);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] *= s_fac[r0 + h + i] * gr;
-                tmem_st8(at, o);
+              for (int k = 0; k < kDaTermsP; ++k) tmem_ld8(at + (uint32_t)(k * R), o[k]);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float f = s_fac[(r0 + h + i) * VG + g];
+#pragma unroll
+                for (int k = 0; k < kDaTermsP; ++k) o[k][i] *= f;
               }
+#pragma unroll
+              for (int k = 0; k < kDaTermsP; ++k) tmem_st8(at + (uint32_t)(k * R), o[k]);
+            }
           }
           tmem_wait_st();
         }
-        softmax_sync<kDaSoft>();                   // (s_fac and s_red may be written again)
+        softmax_sync<kDaSoft>();                   // (s_max and s_inv are written, s_fac and s_red may be again)
+        weigh();
+#pragma unroll
+        for (int r = 0; r < RH; r += 4) {
+          const float4 m = *reinterpret_cast<const float4 *>(s_max + r0 + r);
+          l[r] *= pow2_whole(before[r] - m.x); l[r + 1] *= pow2_whole(before[r + 1] - m.y);
+          l[r + 2] *= pow2_whole(before[r + 2] - m.z); l[r + 3] *= pow2_whole(before[r + 3] - m.w);
+        }
       }
 #pragma unroll
-      for (int r = 0; r < RH; r += 4) {
-        const float4 m = *reinterpret_cast<const float4 *>(s_max + r0 + r);
-        x[r] = ex2(x[r] - m.x); x[r + 1] = ex2(x[r + 1] - m.y); x[r + 2] = ex2(x[r + 2] - m.z); x[r + 3] = ex2(x[r + 3] - m.w);
-        l[r] += x[r]; l[r + 1] += x[r + 1]; l[r + 2] += x[r + 2]; l[r + 3] += x[r + 3];
-      }
+      for (int r = 0; r < RH; ++r) l[r] += p[r];
       if (t > 0) wait(b_empty + 8 * (4 * ((t - 1) & 1) + vg - 1), (uint32_t)(((t - 1) / 2) & 1));   // the weights of the last tile are used up
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
+      for (int g = 0; g < VG; ++g) {
         if (g < vg) {
-          const float f = here ? sg[g] * inv_scale[g] : 0.f;
 #pragma unroll
           for (int h = 0; h < RH; h += 8) {
-            uint32_t w[kDaTermsP][2];
+            uint32_t c[kDaTermsP][2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              __half2 y0 = __floats2half2_rn(x[h + 4 * i] * f, x[h + 4 * i + 1] * f);
-              __half2 y1 = __floats2half2_rn(x[h + 4 * i + 2] * f, x[h + 4 * i + 3] * f);
+              const float *v = w + (h + 4 * i) * VG + g;
+              __half2 y0 = __floats2half2_rn(v[0], v[VG]);
+              __half2 y1 = __floats2half2_rn(v[2 * VG], v[3 * VG]);
 #pragma unroll
-              for (int k = 0; k < kDaTermsP; ++k) { const uint32_t lo2 = e4m3_term(y0); w[k][i] = lo2 | e4m3_term(y1) << 16; }
+              for (int k = 0; k < kDaTermsP; ++k) { const uint32_t lo2 = e4m3_term(y0); c[k][i] = lo2 | e4m3_term(y1) << 16; }
             }
             const int unit = (r0 + h) / 8;         // eight rows: half of a block of 16
             unsigned char *to = ra_smem + L::p(cg, tail) + (unit >> 1) * (kDaTile * 16) + key * 16 + (unit & 1) * 8;
 #pragma unroll
             for (int k = 0; k < kDaTermsP; ++k)
-              *reinterpret_cast<uint2 *>(to + (g * kDaTermsP + k) * (R / 16) * (kDaTile * 16)) = make_uint2(w[k][0], w[k][1]);
+              *reinterpret_cast<uint2 *>(to + (g * kDaTermsP + k) * (R / 16) * (kDaTile * 16)) = make_uint2(c[k][0], c[k][1]);
           }
         }
       }
@@ -570,7 +632,6 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
     softmax_sync<kDaSoft>();
 #pragma unroll 1
     for (int g = 0; g < vg; ++g) {
-      const float ts = g == 0 ? top_scale[0] : g == 1 ? top_scale[1] : g == 2 ? top_scale[2] : top_scale[3];
       const int d = g * 128 + key;                 // (a lane is a number of the group now)
 #pragma unroll
       for (int h = 0; h < RH; h += 8) {
@@ -589,7 +650,8 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int r = r0 + h + i;
-          const float v = nt > 0 && fac[i] != 0.f ? (o[i] + (1.f / kDaStep) * (o2[i] + (1.f / kDaStep) * o3[i])) * ts * fac[i] : 0.f;
+          const float up = __uint_as_float(0x7f000000u - __float_as_uint(s_inv[r * VG + g])) * fac[i];   // 2^k, and the normaliser
+          const float v = nt > 0 && fac[i] != 0.f ? (o[i] + (1.f / kDaStep) * (o2[i] + (1.f / kDaStep) * o3[i])) * up : 0.f;
           if (r < rows) {
             if (whole) a.out[(grow + r) * a.Dv + d] = __float2bfloat16(v);
             else part_out[r * pstride + d] = v;
