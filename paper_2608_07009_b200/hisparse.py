@@ -304,7 +304,10 @@ class _Launch:
         if stream is None:
             self.ptr, self._ctx = torch._C._cuda_getCurrentRawStream(device), None
             return
-        s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
+        s = stream
+        if isinstance(stream, int):
+            # (0 and 1 are the legacy default stream; torch takes a number of 0 for none and makes a stream of its own)
+            s = torch.cuda.ExternalStream(stream, device=device) if stream > 1 else torch.cuda.default_stream(device)
         if s.device.index != device:
             raise ValueError("stream: expected a stream of cuda:%d" % device)
         self.ptr, self._ctx = s.cuda_stream, torch.cuda.stream(s)
