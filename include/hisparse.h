@@ -259,7 +259,8 @@ int hisparse_record_bytes(const hisparse_record_format_t *format, int64_t *bytes
  * beyond num_records writes nothing and sets STATUS_OUT_OF_RANGE in *status_dev (may be NULL).  The slots that are not
  * negative have to differ: two rows for one record leave a mixture of both.  Records that no slot names stay as they are.
  * src_dev, records_dev and every row 16-byte aligned (EINVAL).  Enqueues one kernel; capturable.
- * Every call with a `device` argument makes it current for its own duration and restores the caller's. */
+ * Every call with a `device` argument makes it current for its own duration and restores the caller's.  A pool of no
+ * records (num_records = 0, records_dev may be NULL) is one that every slot or table entry lies beyond. */
 int hisparse_write_records(const hisparse_record_format_t *format, int device, const void *src_dev, int src_type, int64_t src_stride,
                            int64_t count, const int64_t *slots_dev, void *records_dev, int64_t num_records,
                            uint32_t *status_dev, void *stream);

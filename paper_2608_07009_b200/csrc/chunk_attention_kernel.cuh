@@ -161,7 +161,7 @@ chunk_attention_kernel(const RecAtt a, const int dense, const __grid_constant__ 
     const int w = warp - kCaSoftWarps - 2;
     const bool issuer = elect_one();
     bool bad_page = false;
-    const int none = dense ? a.N * dense : (int)a.num_records;   // a row that does not exist
+    const int none = dense ? a.N * dense : ra_none(a);   // a row that does not exist
     // one chunk of 64 keys from j0: as a box where all of it may be read (what lies behind the context in a page may not),
     // eight keys at a time otherwise
     auto bring = [&](const uint32_t dst, const int c, const int j0, const int first, const int r0, const int r1, const uint32_t bar) {

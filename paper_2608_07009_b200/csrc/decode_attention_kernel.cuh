@@ -240,7 +240,7 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
     // ------------------------------------------------------------------ loaders: 32 keys a warp
     const int w = warp - kDaSoftWarps - 2;
     const bool issuer = elect_one();
-    const int none = (int)a.num_records;
+    const int none = ra_none(a);
     bool bad_page = false;
     for (int t = 0; t < nt; ++t) {
       const int st = t & 1, j0 = lo + t * kDaTile;

@@ -185,6 +185,8 @@ __device__ __forceinline__ int32_t ra_resolve(const RecAtt &a, const int32_t e, 
   bad |= e >= 0 && idx >= a.num_records;
   return e < 0 || idx >= a.num_records ? -1 : (int32_t)idx;
 }
+// A row that the pool's tensor maps do not have: filled with zeros.  (The map of an empty pool has one row.)
+__device__ __forceinline__ int32_t ra_none(const RecAtt &a) { return a.num_records > 0 ? (int32_t)a.num_records : 1; }
 __device__ __forceinline__ int32_t ra_index(const RecAtt &a, const int n, const int j, bool &bad) {
   return ra_resolve(a, ra_entry(a, n, j), j, bad);
 }
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(kRaThreads, 1) record_attention_kernel(const R
         const bool boxes = a.box && j0 + kRaTile <= hi;
         const int rows_here = boxes ? (w * 8 % a.box == 0 ? a.box : 0) : 8;
         const int y_box = __shfl_sync(0xffffffffu, idx, 0);
-        const int none = (int)a.num_records;
+        const int none = ra_none(a);
         const int yi = idx < 0 ? none : idx;
         int4 y0, y1;
         y0.x = __shfl_sync(0xffffffffu, yi, 0); y0.y = __shfl_sync(0xffffffffu, yi, 1);

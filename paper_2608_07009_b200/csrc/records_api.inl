@@ -247,7 +247,7 @@ int hisparse_write_records(const hisparse_record_format_t *format, int device, c
   if (device < 0 || count < 0 || num_records < 0 || src_stride < f.D || (!slots_dev && count > num_records)) return HISPARSE_EINVAL;
   if (src_type != HISPARSE_BF16 && src_type != HISPARSE_FP16 && src_type != HISPARSE_FP32) return HISPARSE_EINVAL;
   if (count == 0) return HISPARSE_OK;
-  if (!src_dev || !records_dev) return HISPARSE_EINVAL;
+  if (!src_dev || (!records_dev && num_records)) return HISPARSE_EINVAL;
   if (((uintptr_t)src_dev | (uintptr_t)records_dev) & 15 || src_stride * (src_type == HISPARSE_FP32 ? 4 : 2) % 16) return HISPARSE_EINVAL;
   RecDevice guard(device);
   if (guard.rc) return guard.rc;
@@ -266,7 +266,7 @@ int hisparse_read_records(const hisparse_record_format_t *format, int device, co
   if (rc) return rc;
   if (device < 0 || count < 0 || num_records < 0) return HISPARSE_EINVAL;
   if (count == 0) return HISPARSE_OK;
-  if (!records_dev || !table_dev || !out_dev || ((uintptr_t)records_dev | (uintptr_t)out_dev) & 15) return HISPARSE_EINVAL;
+  if ((!records_dev && num_records) || !table_dev || !out_dev || ((uintptr_t)records_dev | (uintptr_t)out_dev) & 15) return HISPARSE_EINVAL;
   RecDevice guard(device);
   if (guard.rc) return guard.rc;
   const bool few = count <= 148 * 4 * kReadWarps;   // a warp for each entry, and all of them resident
@@ -292,7 +292,7 @@ int hisparse_record_attention(const hisparse_record_attention_t *p, void *worksp
   int rc = ra_geometry(p, &f, &g);
   if (rc) return rc;
   if (p->total_q == 0) return HISPARSE_OK;
-  if (p->device < 0 || !p->records_dev || !p->table_dev || !p->q_dev || !p->out_dev || !p->lse_dev) return HISPARSE_EINVAL;
+  if (p->device < 0 || (!p->records_dev && p->num_records) || !p->table_dev || !p->q_dev || !p->out_dev || !p->lse_dev) return HISPARSE_EINVAL;
   if (((uintptr_t)p->records_dev | (uintptr_t)p->q_dev | (uintptr_t)p->out_dev | (uintptr_t)workspace_dev) & 15) return HISPARSE_EINVAL;
   if (p->q_token_stride % 8 || p->q_head_stride % 8 || p->q_token_stride < 0 || p->q_head_stride < 0) return HISPARSE_EINVAL;
   if (workspace_bytes < g.workspace || (g.workspace && !workspace_dev)) return HISPARSE_EINVAL;
@@ -300,7 +300,8 @@ int hisparse_record_attention(const hisparse_record_attention_t *p, void *worksp
   if (guard.rc) return guard.rc;
   RecAtt a{};
   a.f = f;
-  a.records = static_cast<const uint8_t *>(p->records_dev);
+  // (an empty pool may have no address; the tensor maps want one, of which nothing is read)
+  a.records = static_cast<const uint8_t *>(p->num_records ? p->records_dev : p->q_dev);
   a.num_records = p->num_records;
   a.table = p->table_dev; a.table_stride = p->table_stride; a.room = g.room; a.page = p->page_size;
   a.page_shift = -1;

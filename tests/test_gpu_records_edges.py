@@ -1,0 +1,55 @@
+"""The record operators at the edges of what they are given: pools without records, tables that requests share, batches without
+requests, tensors whose strides along an axis of one mean nothing, contexts near 2^31 keys, errors in the handle's status word."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_07009_b200 as hs
+from oracle import record_oracle as ro
+from paper_2608_07009_b200 import hisparse
+from test_gpu_records import DEV, bf16, check, chunk_case, numbers, pool_of, run_chunk
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# ------------------------------------------------------------------------------------------ pools without records
+
+# the kernel of single tokens over codes, the one of few rows in both formats, pairs on pages, pairs on records laid out once
+PATHS = [(1, 128, 1, 8), (1, 128, 64, 8), (1, 0, 1, 8), (1, 0, 64, 8), (3, 128, 16, 8), (3, 0, 16, 8), (20, 0, 64, 8), (30, 128, 16, 8), (30, 0, 7, 8)]
+
+
+@pytest.mark.parametrize("m,Dq,page,H", PATHS)
+@pytest.mark.parametrize("address", [False, True])
+def test_attention_over_an_empty_pool(m, Dq, page, H, address):
+    """Nothing is read, not even where the address has NaN records behind it."""
+    fmt, D, Dv, K = hs.RecordFormat(144, Dq), 144, 128, 150
+    pool = torch.full((400, fmt.entry_bytes), 0x7F, dtype=torch.uint8, device=DEV)
+    ptr = pool.data_ptr() if address else pool[:0].clone().data_ptr()
+    q, table = torch.randn((2 * m, H, D), device=DEV).to(torch.bfloat16), torch.full((2, -(-K // page)), -1, dtype=torch.int32, device=DEV)
+    status = i32([0])
+    args = lambda: (fmt, ptr, 0, 0, table, q, Dv, 0.1, page, i32([0, m, 2 * m]), i32([K, 9]), m, K, 1, None, None, None, status, None)  # noqa: E731
+    for entries, want in ((None, 0), (torch.arange(table.shape[1], dtype=torch.int32, device=DEV), hs.STATUS_OUT_OF_RANGE)):
+        if entries is not None:
+            table[0] = entries
+        out, lse = hisparse._attend(*args())
+        assert torch.all(out == 0) and torch.all(torch.isneginf(lse)) and status.item() == want
+
+
+def test_writing_and_reading_an_empty_pool():
+    fmt = hs.RecordFormat(144, 128)
+    pool = torch.empty((0, fmt.entry_bytes), dtype=torch.uint8, device=DEV)
+    x, status = torch.randn((3, 144), device=DEV).to(torch.bfloat16), i32([0])
+    slots = torch.tensor([-1, -1, -1], device=DEV)
+    hs.write_records(fmt, x, pool, slots=slots, status=status)
+    assert torch.all(hs.read_records(fmt, pool, i32([[-1, -1]]), status=status) == 0) and status.item() == 0
+    assert torch.all(hs.read_records(fmt, pool, i32([[-1, 0]]), status=status) == 0) and status.item() == hs.STATUS_OUT_OF_RANGE
+    status.zero_()
+    slots[1] = 0
+    hs.write_records(fmt, x, pool, slots=slots, status=status)
+    assert status.item() == hs.STATUS_OUT_OF_RANGE
+    out, lse = hs.record_attention(fmt, pool, torch.full((2, 5), -1, dtype=torch.int32, device=DEV), x[:2, None].expand(2, 4, 144), 128, 1.0)
+    assert torch.all(out == 0) and torch.all(torch.isneginf(lse))
