@@ -331,6 +331,8 @@ int hisparse_record_attention(const hisparse_record_attention_t *problem, void *
 
 /* Sticky status bits accumulated by the device code (HISPARSE_STATUS_*).  Synchronises the device. */
 int hisparse_status(hisparse_t *h, uint32_t *bits);
+/* Device address of that word, for the status_dev of record operators over the handle's cache; NULL without a handle. */
+uint32_t *hisparse_status_word(const hisparse_t *h);
 int hisparse_clear_status(hisparse_t *h);
 
 /* Copies one (request, layer)'s metadata to host buffers; any pointer may be NULL.  slot_pos [B]

@@ -664,6 +664,8 @@ int hisparse_status(hisparse_t *h, uint32_t *bits) {
   return HISPARSE_OK;
 }
 
+uint32_t *hisparse_status_word(const hisparse_t *h) { return h ? h->d.status : nullptr; }
+
 int hisparse_clear_status(hisparse_t *h) {
   if (!h) return HISPARSE_EINVAL;
   HS_CUDA(cudaSetDevice(h->device));

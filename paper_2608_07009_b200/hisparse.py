@@ -32,7 +32,7 @@ EXPORTS = [
     "hisparse_scatter_read_probe", "hisparse_resolve_noalloc", "hisparse_strerror", "hisparse_last_cuda_error",
     "hisparse_attention_workspace_bytes", "hisparse_sparse_attention",
     "hisparse_record_bytes", "hisparse_write_records", "hisparse_read_records",
-    "hisparse_record_attention_workspace_bytes", "hisparse_record_attention",
+    "hisparse_record_attention_workspace_bytes", "hisparse_record_attention", "hisparse_status_word",
 ]
 
 
@@ -111,6 +111,7 @@ def lib() -> ctypes.CDLL:
             "hisparse_gather": ([vp, i32, vp, vp, vp], i32),
             "hisparse_gather_check": ([vp, i32, vp, vp, vp, vp], i32),
             "hisparse_status": ([vp, P(u32)], i32),
+            "hisparse_status_word": ([vp], vp),
             "hisparse_clear_status": ([vp], i32),
             "hisparse_dump_state": ([vp, i32, i32, vp, vp, vp, vp, P(i64), P(i64), P(u32)], i32),
             "hisparse_load_state": ([vp, i32, i32, vp, vp, u32], i32),
@@ -284,8 +285,9 @@ def _records_of(fmt: RecordFormat, records):
 
 
 def _status_of(status, device: int):
-    if status is None:
-        return None
+    """Address of a status word: None, an address (a handle's word) or one int32 on the device."""
+    if status is None or isinstance(status, int):
+        return status
     import torch
     if status.dtype not in (torch.int32, torch.uint32) or status.numel() != 1 or not status.is_cuda or status.get_device() != device:
         raise ValueError("status: expected one int32 on cuda:%d" % device)
@@ -540,9 +542,10 @@ class HiSparse:
 
     # ---- records of numbers (RecordFormat with this handle's entry_bytes) ----
     def _pool_of(self, layer: int, fmt: "RecordFormat"):
+        """(address, records, device, address of the handle's status word)"""
         if fmt.entry_bytes != self.E:
             raise ValueError("%r has %d bytes, the handle's records %d" % (fmt, fmt.entry_bytes, self.E))
-        return self.layer_pool(layer), self.N * (self.B + 1), self.device
+        return self.layer_pool(layer), self.N * (self.B + 1), self.device, lib().hisparse_status_word(self._h)
 
     def append_values(self, fmt: "RecordFormat", values, stream=None) -> None:
         """append of bf16, fp16 or fp32 numbers [N][L][dims], written as records of `fmt`."""
@@ -557,22 +560,24 @@ class HiSparse:
             self.append(records, stream=on.ptr)
 
     def gather_values(self, layer: int, fmt: "RecordFormat", slot_table, out=None, stream=None):
-        """bf16 [N][k][dims]: the numbers of the records that a slot table addresses (gather, expanded)."""
-        ptr, count, device = self._pool_of(layer, fmt)
+        """bf16 [N][k][dims]: the numbers of the records that a slot table addresses (gather, expanded).  A slot beyond the
+        cache gives zeros and STATUS_OUT_OF_RANGE in status()."""
+        ptr, count, device, word = self._pool_of(layer, fmt)
         with _Launch(stream, device) as on:
             self.join(on.ptr)
-            return _read(fmt, ptr, count, device, slot_table, out, None, stream)
+            return _read(fmt, ptr, count, device, slot_table, out, word, stream)
 
     def record_attention(self, layer: int, fmt: "RecordFormat", q, slot_table, value_dims: int, scale: float, out=None, lse=None,
                          workspace=None, stream=None):
-        """record_attention over this layer's cache: any number of heads, either record format, bf16 out."""
-        ptr, count, device = self._pool_of(layer, fmt)
+        """record_attention over this layer's cache: any number of heads, either record format, bf16 out; errors of the kernels
+        appear in status()."""
+        ptr, count, device, word = self._pool_of(layer, fmt)
         if tuple(slot_table.shape) != (self.N, self.k):
             raise ValueError("slot_table: expected [%d][%d]" % (self.N, self.k))
         with _Launch(stream, device) as on:
             self.join(on.ptr)                # a prefetch replay or a write-through may still be filling this layer's cache
             return _attend(fmt, ptr, count, device, slot_table, q, value_dims, scale, 1, None, None, 1, 0, 0, out, lse, workspace,
-                           None, stream)
+                           word, stream)
 
     # ---- consumer stand-ins ----
     def layer_pool(self, layer: int) -> int:

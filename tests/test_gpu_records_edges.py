@@ -53,3 +53,30 @@ def test_writing_and_reading_an_empty_pool():
     assert status.item() == hs.STATUS_OUT_OF_RANGE
     out, lse = hs.record_attention(fmt, pool, torch.full((2, 5), -1, dtype=torch.int32, device=DEV), x[:2, None].expand(2, 4, 144), 128, 1.0)
     assert torch.all(out == 0) and torch.all(torch.isneginf(lse))
+
+
+# ------------------------------------------------------------------------------------------ the handle's status word
+
+def test_errors_over_a_handles_cache_reach_its_status():
+    N, L, B, k, D = 2, 2, 16, 8, 144
+    fmt = hs.RecordFormat(D, 128)
+    hist = [hs.HostHistory(L, 40, fmt.entry_bytes) for _ in range(N)]
+    gpu = hs.HiSparse(N, L, 1, B, k, fmt.entry_bytes, [40] * N, [30] * N, hist)
+    try:
+        q, rows = torch.randn((N, 4, D), device=DEV).to(torch.bfloat16), N * (B + 1)
+        table = torch.arange(N * k, dtype=torch.int32, device=DEV).reshape(N, k)
+        gpu.gather_values(1, fmt, table)
+        gpu.record_attention(1, fmt, q, table, 128, 0.1)
+        assert gpu.status() == 0
+        for beyond in (rows, 2147483647):
+            table[1, 3] = beyond
+            assert torch.all(gpu.gather_values(1, fmt, table)[1, 3] == 0)
+            assert gpu.status() == hs.STATUS_OUT_OF_RANGE
+            gpu.clear_status()
+            gpu.record_attention(1, fmt, q, table, 128, 0.1)
+            assert gpu.status() == hs.STATUS_OUT_OF_RANGE
+            gpu.clear_status()
+    finally:
+        gpu.close()
+        for h in hist:
+            h.free()
