@@ -113,7 +113,8 @@ chunk_attention_kernel(const RecAtt a, const int dense, const __grid_constant__ 
   const int row0 = pair0 + (int)rank * kCaRows, rows = min(kCaRows, rq.qlen * a.H - row0);   // of this SM, may be none
   const int hi_all = min(rq.kv, ra_limit(a, rq, (pair0 + pair_rows - 1) / a.H));
   const int tiles_all = (hi_all + kCaTile - 1) / kCaTile, per = (tiles_all + a.splits - 1) / a.splits;
-  const int lo = (int)split * per * kCaTile, hi = min(hi_all, lo + per * kCaTile);
+  // (bounds in tiles first: a split's end in keys may lie beyond 2^31)
+  const int lo = min((int)split * per, tiles_all) * kCaTile, hi = min(hi_all, min(((int)split + 1) * per, tiles_all) * kCaTile);
   const int nt = hi > lo ? (hi - lo + kCaTile - 1) / kCaTile : 0;
 
   bool dead = false;

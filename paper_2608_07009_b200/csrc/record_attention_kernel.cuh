@@ -309,7 +309,8 @@ __global__ void __launch_bounds__(kRaThreads, 1) record_attention_kernel(const R
   const int hi_all = min(rq.kv, ra_limit(a, rq, (row0 + rows - 1) / a.H));
   const int lo_full = min(rq.kv, ra_limit(a, rq, row0 / a.H));             // keys below are seen by every row
   const int tiles_all = (hi_all + kRaTile - 1) / kRaTile, per = (tiles_all + a.splits - 1) / a.splits;
-  const int lo = (int)split * per * kRaTile, hi = min(hi_all, lo + per * kRaTile);
+  // (bounds in tiles first: a split's end in keys may lie beyond 2^31)
+  const int lo = min((int)split * per, tiles_all) * kRaTile, hi = min(hi_all, min(((int)split + 1) * per, tiles_all) * kRaTile);
   const int nt = hi > lo ? (hi - lo + kRaTile - 1) / kRaTile : 0;
 
   bool dead = false;                              // a bounded wait ran out: finish without waiting

@@ -80,3 +80,24 @@ def test_errors_over_a_handles_cache_reach_its_status():
         gpu.close()
         for h in hist:
             h.free()
+
+
+# ------------------------------------------------------------------------------------------ contexts near 2^31 keys
+
+@pytest.mark.parametrize("m,H,Dq", [(1, 4, 0), (2, 3, 128), (20, 4, 0)])
+def test_the_longest_context_that_is_taken(m, H, Dq):
+    """2^31 - 1024 keys of which a few pages are there, the last one among them: the last split ends at its context's end."""
+    rng = np.random.default_rng(m)
+    D, page = 128, 1024
+    width = 2 ** 21 - 1
+    raw, num = pool_of(rng, 3 * page, D, Dq)
+    table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    for at, p in ((0, 2), (1234567, 0), (width - 1, 1)):
+        table[0, at] = p
+    K = width * page
+    q = ro.bf16_values(ro.round_to_bf16(rng.standard_normal((m, H, D))))
+    out, lse = hs.chunk_attention(hs.RecordFormat(D, Dq), torch.from_numpy(raw).to(DEV), table, i32([K]), bf16(q).to(DEV), i32([0, m]), 128, 0.1,
+                                  page_size=page, max_q_len=m)
+    keys = np.concatenate([num[2 * page:], num[:page], num[page:2 * page]])
+    ref = [ro.attention(keys, np.arange(3 * page) < 3 * page - m + t + 1, q[t], 128, 0.1) for t in range(m)]
+    check(out, lse, np.stack([r[0] for r in ref]), np.stack([r[1] for r in ref]), q, num, 0.1, D)
