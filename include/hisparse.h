@@ -256,7 +256,8 @@ int hisparse_record_bytes(const hisparse_record_format_t *format, int64_t *bytes
 
 /* Writes `count` rows of D numbers as records: row i, at src_dev + i * src_stride elements, becomes record slots_dev[i]
  * (int64; NULL: record i) of records_dev, uint8 [num_records][E].  A negative slot is padding and writes nothing; one
- * beyond num_records writes nothing and sets STATUS_OUT_OF_RANGE in *status_dev (may be NULL).  The slots that are not
+ * beyond num_records writes nothing and sets STATUS_OUT_OF_RANGE in *status_dev (may be NULL).  src_stride 0 writes one row
+ * to every slot, otherwise it is at least D.  The slots that are not
  * negative have to differ: two rows for one record leave a mixture of both.  Records that no slot names stay as they are.
  * src_dev, records_dev and every row 16-byte aligned (EINVAL).  Enqueues one kernel; capturable.
  * Every call with a `device` argument makes it current for its own duration and restores the caller's.  A pool of no
@@ -299,7 +300,7 @@ typedef struct {
   hisparse_record_format_t format;  /* dims at most 576 */
   const void *records_dev;          /* uint8 [num_records][E], 16-byte aligned */
   int64_t num_records;
-  const int32_t *table_dev;         /* [num_requests] rows of table_width entries, table_stride apart */
+  const int32_t *table_dev;         /* [num_requests] rows of table_width entries, table_stride apart (0: one row for all) */
   int64_t table_stride;
   int32_t table_width;              /* table_width * page_size at most 2^31 - 1024 */
   int32_t page_size;

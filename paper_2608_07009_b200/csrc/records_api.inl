@@ -106,7 +106,7 @@ int ra_geometry(const hisparse_record_attention_t *p, RecFmt *f, RaGeom *g) {
   if (f->D > kRaMaxDims || !(p->value_dims == 128 || p->value_dims == 256 || p->value_dims == 512) || p->value_dims > f->D)
     return HISPARSE_EINVAL;
   if (p->num_requests < 1 || p->num_heads < 1 || p->num_heads > HISPARSE_MAX_HEADS || p->page_size < 1 || p->table_width < 1 ||
-      p->table_stride < p->table_width || p->num_records < 0 || p->num_records > INT32_MAX || p->total_q < 0 || p->max_q_len < 1)
+      (p->table_stride < p->table_width && p->table_stride != 0) || p->num_records < 0 || p->num_records > INT32_MAX || p->total_q < 0 || p->max_q_len < 1)
     return HISPARSE_EINVAL;
   // (the kernels count keys and rows in 32 bits and look a few tiles ahead)
   if ((int64_t)p->table_width * p->page_size > INT32_MAX - 1023 || (int64_t)p->max_q_len * p->num_heads > INT32_MAX - 1023) return HISPARSE_EINVAL;
@@ -244,7 +244,7 @@ int hisparse_write_records(const hisparse_record_format_t *format, int device, c
   RecFmt f;
   const int rc = rec_format(format, &f);
   if (rc) return rc;
-  if (device < 0 || count < 0 || num_records < 0 || src_stride < f.D || (!slots_dev && count > num_records)) return HISPARSE_EINVAL;
+  if (device < 0 || count < 0 || num_records < 0 || (src_stride < f.D && src_stride != 0) || (!slots_dev && count > num_records)) return HISPARSE_EINVAL;
   if (src_type != HISPARSE_BF16 && src_type != HISPARSE_FP16 && src_type != HISPARSE_FP32) return HISPARSE_EINVAL;
   if (count == 0) return HISPARSE_OK;
   if (!src_dev || (!records_dev && num_records)) return HISPARSE_EINVAL;

@@ -392,8 +392,9 @@ def _attend(fmt, ptr, count, device, table, q, value_dims, scale, page_size, q_s
         kv_ptr = _on_device(kv_len, int32, device, "kv_len")
         if kv_len.numel() != N:
             raise ValueError("kv_len: expected %d entries, got %d" % (N, kv_len.numel()))
+    # (an axis of one has any stride)
     p = _RecordAttention(device, fmt._c, ptr, count, table.data_ptr(), table.stride(0) if N > 1 else width, width, page_size, N, H,
-                         value_dims, q.data_ptr(), q_token, q_head, T, start_ptr, max_q_len, kv_ptr, max_kv_len, causal, scale,
+                         value_dims, q.data_ptr(), q_token if T > 1 else 0, q_head if H > 1 else 0, T, start_ptr, max_q_len, kv_ptr, max_kv_len, causal, scale,
                          None, None, _status_of(status, device))
     need = ctypes.c_size_t()
     rc = lib().hisparse_record_attention_workspace_bytes(p, need)

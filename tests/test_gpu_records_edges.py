@@ -101,3 +101,44 @@ def test_the_longest_context_that_is_taken(m, H, Dq):
     keys = np.concatenate([num[2 * page:], num[:page], num[page:2 * page]])
     ref = [ro.attention(keys, np.arange(3 * page) < 3 * page - m + t + 1, q[t], 128, 0.1) for t in range(m)]
     check(out, lse, np.stack([r[0] for r in ref]), np.stack([r[1] for r in ref]), q, num, 0.1, D)
+
+
+# ------------------------------------------------------------------------------------------ strides
+
+@pytest.mark.parametrize("Dq", [0, 128])
+@pytest.mark.parametrize("m", [1, 2, 30])
+def test_requests_that_share_a_table_row(m, Dq):
+    rng = np.random.default_rng(m + Dq)
+    D, N, page, K = 144, 3, 16, 100
+    raw, num, table, cs, q, q_start = chunk_case(rng, [m] * N, [K] * N, 8, D, Dq, page)
+    row = torch.from_numpy(table[:1]).to(DEV)
+    args = (hs.RecordFormat(D, Dq), torch.from_numpy(raw).to(DEV))
+    rest = (i32([K] * N), bf16(q).to(DEV), torch.from_numpy(q_start).to(DEV), 128, 0.1)
+    out, lse = hs.chunk_attention(*args, row.expand(N, -1), *rest, page_size=page, max_q_len=m)
+    out_ref, lse_ref, _ = ro.chunk(num, np.repeat(table[:1], N, 0), cs, q, q_start, 128, 0.1, page)
+    check(out[:-2], lse[:-2], out_ref[:-2], lse_ref[:-2], q, num, 0.1, D)
+
+
+def test_axes_of_one_with_any_stride():
+    rng = np.random.default_rng(1)
+    D, K = 144, 40
+    raw, num = pool_of(rng, K, D, 128)
+    pool, table = torch.from_numpy(raw).to(DEV), torch.arange(K, dtype=torch.int32, device=DEV)[None]
+    q = ro.bf16_values(ro.round_to_bf16(rng.standard_normal((1, 1, D))))
+    ref = ro.attention(num, np.ones(K, bool), q[0], 128, 0.1)
+    flat = bf16(q).to(DEV).reshape(-1)
+    for strides in ((3, 5, 1), (D, 1, 1), (1001, 7, 1)):
+        out, lse = hs.record_attention(hs.RecordFormat(D, 128), pool, table, flat.as_strided((1, 1, D), strides), 128, 0.1)
+        check(out, lse, ref[0][None], ref[1][None], q, num, 0.1, D)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_one_row_written_to_many_slots(dtype):
+    fmt = hs.RecordFormat(576, 512)
+    row = torch.randn((1, 576), device=DEV).to(dtype)
+    pool = torch.zeros((20, fmt.entry_bytes), dtype=torch.uint8, device=DEV)
+    slots = torch.tensor([3, 0, -1, 19, 7], device=DEV)
+    hs.write_records(fmt, row.expand(5, 576), pool, slots=slots)
+    want = np.zeros((20, fmt.entry_bytes), dtype=np.uint8)
+    want[[3, 0, 19, 7]] = ro.encode(row.double().cpu().numpy(), 512)
+    assert np.array_equal(pool.cpu().numpy(), want)
