@@ -392,6 +392,9 @@ def _attend(fmt, ptr, count, device, table, q, value_dims, scale, page_size, q_s
         kv_ptr = _on_device(kv_len, int32, device, "kv_len")
         if kv_len.numel() != N:
             raise ValueError("kv_len: expected %d entries, got %d" % (N, kv_len.numel()))
+    if N == 0 and (T == 0 or q_start is not None):   # no request, no row to write
+        out = q.new_empty((T, H, value_dims)) if out is None else out
+        return out, q.new_empty((T, H), dtype=f32) if lse is None else lse
     # (an axis of one has any stride)
     p = _RecordAttention(device, fmt._c, ptr, count, table.data_ptr(), table.stride(0) if N > 1 else width, width, page_size, N, H,
                          value_dims, q.data_ptr(), q_token if T > 1 else 0, q_head if H > 1 else 0, T, start_ptr, max_q_len, kv_ptr, max_kv_len, causal, scale,
@@ -441,7 +444,8 @@ def chunk_attention(fmt: RecordFormat, records, page_table, kv_len, q, q_start, 
     (int32 [N + 1]) of q, bf16 [tokens][H][dims], and the last ones of its kv_len[n] keys (int32 [N]), which are records
     page_table[n][j // page_size] * page_size + j % page_size (int32 [N][pages], negative = absent) of `records`.  With
     `causal`, token t of m sees the keys up to kv_len[n] - m + t, its own.  max_q_len and max_kv_len
-    (0: the table's width) bound chunks and contexts.  Returns (out bf16 [tokens][H][value_dims], lse float32 [tokens][H]);
+    (0: the table's width) bound chunks and contexts.  A batch of no requests writes nothing; a table without entries is
+    refused.  Returns (out bf16 [tokens][H][value_dims], lse float32 [tokens][H]);
     rows that belong to no request are left as they were."""
     ptr, count, device = _records_of(fmt, records)
     return _attend(fmt, ptr, count, device, page_table, q, value_dims, scale, page_size, q_start, kv_len, max_q_len, max_kv_len,

@@ -142,3 +142,20 @@ def test_one_row_written_to_many_slots(dtype):
     want = np.zeros((20, fmt.entry_bytes), dtype=np.uint8)
     want[[3, 0, 19, 7]] = ro.encode(row.double().cpu().numpy(), 512)
     assert np.array_equal(pool.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------------------------------ batches without requests
+
+def test_no_requests():
+    fmt = hs.RecordFormat(144, 128)
+    pool = torch.zeros((8, fmt.entry_bytes), dtype=torch.uint8, device=DEV)
+    none = torch.zeros((0, 5), dtype=torch.int32, device=DEV)
+    q = torch.zeros((3, 4, 144), dtype=torch.bfloat16, device=DEV)
+    out, lse = hs.record_attention(fmt, pool, none, q[:0], 128, 1.0)
+    assert out.shape == (0, 4, 128) and out.dtype == torch.bfloat16 and lse.shape == (0, 4) and lse.dtype == torch.float32
+    mine = torch.full((3, 4, 128), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((3, 4), 7.0, device=DEV)
+    got = hs.chunk_attention(fmt, pool, none, i32([]), q, i32([0]), 128, 1.0, page_size=1, max_q_len=1, out=mine[0], lse=mine[1])
+    assert got[0] is mine[0] and got[1] is mine[1] and torch.all(mine[0] == 7) and torch.all(mine[1] == 7)
+    assert hs.chunk_attention(fmt, pool, none, i32([]), q, i32([0]), 128, 1.0, page_size=1, max_q_len=1)[0].shape == (3, 4, 128)
+    with pytest.raises(hs.HiSparseError):                           # a row a request, and no request for the rows
+        hs.record_attention(fmt, pool, none, q, 128, 1.0)
