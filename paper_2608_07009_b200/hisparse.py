@@ -233,6 +233,13 @@ def resolve_noalloc(state: ExternalState, sel, slot_table, hits, misses, status=
 #
 # These calls take a few microseconds on the device, so the checks in front of them are kept to plain attribute reads.
 
+def _int32(*numbers) -> None:
+    """Refuses what an int32 field would cut off."""
+    for n in numbers:
+        if not -(1 << 31) <= n < 1 << 31:
+            raise HiSparseError(EINVAL, "%d does not fit 32 bits" % n)
+
+
 class RecordFormat:
     """Layout of a record of `dims` numbers: the first `quant_dims` (a multiple of 128) as e4m3 codes with a power-of-two
     scale per 128, the others bf16; quant_dims = 0 is the plain bf16 record.  `entry_bytes` is its size, and what a
@@ -244,6 +251,7 @@ class RecordFormat:
     def __new__(cls, dims: int, quant_dims: int = 0):
         f = cls._made.get((dims, quant_dims))
         if f is None:
+            _int32(dims, quant_dims)
             f = object.__new__(cls)
             f.dims, f.quant_dims, f._c = dims, quant_dims, _RecordFormat(dims, quant_dims)
             n = ctypes.c_int64()
@@ -380,6 +388,7 @@ def _attend(fmt, ptr, count, device, table, q, value_dims, scale, page_size, q_s
         raise ValueError("table: expected an int32 tensor [requests][entries] on cuda:%d" % device)
     if not (q.dtype is bf16 and q.is_cuda and q.dim() == 3 and q.get_device() == device and q.shape[2] == fmt.dims and q.stride(2) == 1):
         raise ValueError("q: expected a bfloat16 tensor [tokens][heads][%d] on cuda:%d" % (fmt.dims, device))
+    _int32(value_dims, page_size, max_q_len, max_kv_len)
     N, width = table.shape
     T, H, _ = q.shape
     q_token, q_head, _ = q.stride()

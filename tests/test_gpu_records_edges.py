@@ -159,3 +159,19 @@ def test_no_requests():
     assert hs.chunk_attention(fmt, pool, none, i32([]), q, i32([0]), 128, 1.0, page_size=1, max_q_len=1)[0].shape == (3, 4, 128)
     with pytest.raises(hs.HiSparseError):                           # a row a request, and no request for the rows
         hs.record_attention(fmt, pool, none, q, 128, 1.0)
+
+
+# ------------------------------------------------------------------------------------------ numbers beyond 32 bits
+
+def test_sizes_beyond_32_bits_are_refused():
+    """They used to be cut to their low 32 bits: 2^32 + 1 tokens became 1."""
+    fmt = hs.RecordFormat(144, 128)
+    pool = torch.zeros((64, fmt.entry_bytes), dtype=torch.uint8, device=DEV)
+    q = torch.zeros((2, 16, 144), dtype=torch.bfloat16, device=DEV)
+    sizes = dict(value_dims=128, page_size=4, max_q_len=1, max_kv_len=8)
+    for name in sizes:
+        for more in (1 << 32, -(1 << 32)):
+            args = dict(sizes, **{name: sizes[name] + more})
+            with pytest.raises(hs.HiSparseError) as e:
+                hs.chunk_attention(fmt, pool, i32([[0, 1], [2, 3]]), i32([8, 8]), q, i32([0, 1, 2]), args.pop("value_dims"), 1.0, **args)
+            assert e.value.code == hisparse.EINVAL

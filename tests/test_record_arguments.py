@@ -1,5 +1,7 @@
-"""Arguments of the record operators that need no device: strides of 0."""
+"""Arguments of the record operators that need no device: strides of 0, numbers beyond 32 bits."""
 import ctypes
+
+import pytest
 
 from test_record_oracle import problem
 
@@ -12,3 +14,11 @@ def test_one_table_row_for_all_requests():
     assert call(problem(hs, table_stride=0), m) == hs.OK and m.value == n.value
     for stride in (1, 9, -1, -10):
         assert call(problem(hs, table_stride=stride), n) == hs.EINVAL
+
+
+def test_formats_beyond_32_bits():
+    from paper_2608_07009_b200 import hisparse as hs
+    for dims, quant in (((1 << 32) + 576, 512), (576, (1 << 32) + 512), (576 - (1 << 32), 512), (1 << 31, 0)):
+        with pytest.raises(hs.HiSparseError) as e:
+            hs.RecordFormat(dims, quant)
+        assert e.value.code == hs.EINVAL
