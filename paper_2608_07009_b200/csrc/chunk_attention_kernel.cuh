@@ -466,8 +466,7 @@ chunk_attention_kernel(const RecAtt a, const int dense, const __grid_constant__ 
   }
   // both products over (the first SM's commits arrive here as well) before the tensor memory goes and the pair parts
   if (warp == kCaSoftWarps) { wait(b_end, 0); wait(b_end + 8, 0); }
-  if (dead && lane == 0 && a.status) atomicOr(a.status, HISPARSE_STATUS_TIMEOUT);
-  __syncthreads();
+  if (__syncthreads_or(dead)) ra_gave_up(a.status);
   // (relaxed: nothing is handed over, and a release would wait for the output to reach memory)
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
   if (warp == kCaSoftWarps) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));

@@ -138,6 +138,7 @@ __device__ __forceinline__ float4 peer_f32x4(const uint32_t addr, const uint32_t
 template <int R>
 __device__ __forceinline__ void da_merge(const RecAtt &a, const int64_t grow, const int rows, const uint32_t rank, const uint32_t o,
                                          const uint32_t m, const uint32_t l, float *w) {
+  __syncwarp();                                   // (lanes whose waits ran out one by one)
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   const int tid = threadIdx.x;
   if (tid < rows) {
@@ -663,8 +664,7 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
   }
   if (cluster) da_merge<R>(a, rq.q0 * a.H + row0, rows, split, sbase, sbase + L::max(cg, tail, vg), sbase + L::qs(cg, tail, vg),
                            reinterpret_cast<float *>(ra_smem + L::p(cg, tail)));
-  if (dead && lane == 0 && a.status) atomicOr(a.status, HISPARSE_STATUS_TIMEOUT);
-  __syncthreads();
+  if (__syncthreads_or(dead)) ra_gave_up(a.status);
   if (warp == kDaSoftWarps) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
 }
 

@@ -104,6 +104,13 @@ __device__ __forceinline__ bool mbar_wait_quick(const uint32_t bar, const uint32
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done ? true : mbar_wait_bounded(bar, parity);
 }
+// The end of a block in which a bounded wait ran out (all its threads): the status, and a bounded time in which copies that are
+// still in flight land, before its shared memory goes to another block.
+__device__ __noinline__ void ra_gave_up(uint32_t *status) {
+  if (threadIdx.x == 0 && status) atomicOr(status, HISPARSE_STATUS_TIMEOUT);
+  const uint64_t t0 = global_ns();
+  for (int i = 0; i < 10000 && global_ns() - t0 < 1000000; ++i) __nanosleep(1000);
+}
 __device__ __forceinline__ void mbar_arrive_tx(const uint32_t bar, const uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -522,7 +529,7 @@ __global__ void __launch_bounds__(kRaThreads, 1) record_attention_kernel(const R
       __syncwarp();
     }
     if (issuer) umma_commit(b_end);               // everything issued has finished before the tensor memory is freed
-    mbar_wait_bounded(b_end, 0);
+    if (!mbar_wait_bounded(b_end, 0)) dead = true;
     __syncwarp();
   } else if (warp == kRaSoftmaxWarps + 1) {
     // ------------------------------------------------------------------ O^T += V^T P^T
@@ -547,7 +554,7 @@ __global__ void __launch_bounds__(kRaThreads, 1) record_attention_kernel(const R
       __syncwarp();
     }
     if (issuer) umma_commit(b_end + 8);
-    mbar_wait_bounded(b_end + 8, 0);
+    if (!mbar_wait_bounded(b_end + 8, 0)) dead = true;
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ softmax
@@ -733,8 +740,7 @@ __global__ void __launch_bounds__(kRaThreads, 1) record_attention_kernel(const R
       }
     }
   }
-  if (dead && lane == 0 && a.status) atomicOr(a.status, HISPARSE_STATUS_TIMEOUT);
-  __syncthreads();
+  if (__syncthreads_or(dead)) ra_gave_up(a.status);
   if (warp == kRaSoftmaxWarps)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols));
 }
