@@ -12,8 +12,8 @@
 //            so far, the weight and the size of one and the same record, which comes to lie above 2^lift and at most at 2^8, with
 //            lift such that all keys together are off by at most 2^-8 of the largest p max |value| of the group, no more than
 //            bf16's rounding: 0 for 2048 keys, 6 for 131072, the most that this kernel is given.  A small lift leaves the
-//            maximum room, so that it moves for a fraction of the tiles (8 of 64; 32 x 32768 keys take 157 us with a lift of 4,
-//            150 with 3, 141 with 0).  A group of zeros has scale 1 and no size: it does not count, for which the codes of
+//            maximum room, so that it moves for a fraction of the tiles (13 of 64; 32 x 32768 keys take 152 us with a lift of 4,
+//            141 if it never moves).  A group of zeros has scale 1 and no size: it does not count, for which the codes of
 //            groups with that scale are looked at.  (With the largest scale in place of the largest p scale, 142 us, a record of
 //            zeros, or a large one that is not attended, took the weights of all others below the terms' reach.)  The running
 //            maximum of a row is a whole number, so that k moves with it exactly.
@@ -21,10 +21,10 @@
 // Splits of a context meet in a cluster where there are 2, 4 or 8: every block leaves its O, m and l in shared memory and merges
 // a share of the numbers out of all of them, which saves the second kernel and its 2 x 33 KB a block through memory.
 // Both products are transposed as there: 128 keys or 128 numbers are M, R query rows times their terms are N.
-// 32 requests x 32768 keys of 656 bytes, 16 heads: 157 us, 4.3 TB/s, bound by the TMA's rows (each 128 bytes of such a record
-// lie in two lines; loads alone take 129 us) and by the tiles whose maxima move; with stages released as a whole instead of by
-// group 14 us more.  32 x 2048 keys through a slot table: 22.5 us, where four-row gathers (25 cycles
-// each) and a block's start and end count as much as its four tiles.
+// 32 requests x 32768 keys of 656 bytes, 16 heads: 152 us, 4.5 TB/s, bound by the TMA's rows (each 128 bytes of such a record
+// lie in two lines; loads alone take 129 us) and by the softmax warps (3000 cycles a tile, 2600 more where maxima move); with
+// stages released as a whole instead of by group 14 us more.  32 x 2048 keys through a slot table: 22.1 us, where four-row
+// gathers (25 cycles each) and a block's start and end count as much as its four tiles.
 //   tile     128 keys: [group][key][128 bytes] of codes (K-major for S^T, MN-major for O^T) and [key][128 bytes] of tail, by TMA
 //            boxes or four-row gathers; two stages
 //   warps    0-7 softmax, two threads a key with half of the rows each (the key's scales come by plain loads a tile ahead;
@@ -465,12 +465,19 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
         for (int i = 0; i < 8; ++i) x[h + i] = here ? acc[i] * qs[i] + (tail ? s3[i] * a.scale_log2e : 0.f) : -INFINITY;
       }
       // the scales that the weights are measured with: none where the group is zeros
+      // (one branch for all groups: one each took 250 cycles a tile)
       float se[VG];
+      bool ones = false;
 #pragma unroll
       for (int g = 0; g < VG; ++g) {
         se[g] = here && g < vg ? sg[g] : 0.f;
-        if (se[g] == 1.f) {
-          wait(b_full + 8 * st, (uint32_t)((t / 2) & 1));   // (it has come; the wait makes the codes visible to this thread)
+        ones |= se[g] == 1.f;
+      }
+      if (ones) {
+        wait(b_full + 8 * st, (uint32_t)((t / 2) & 1));   // (it has come; the wait makes the codes visible to this thread)
+#pragma unroll
+        for (int g = 0; g < VG; ++g) {
+          if (se[g] != 1.f) continue;
           const unsigned char *row = ra_smem + (uint32_t)st * stage_bytes + g * kDaChunk + key * 128;
           uint32_t some = 0;
 #pragma unroll 1
@@ -542,8 +549,9 @@ decode_attention_kernel(const RecAtt a, const float lift, const int cluster, con
         if (t > 0) {
           wait(b_empty + 8 * (4 * ((t - 1) & 1) + vg - 1), (uint32_t)(((t - 1) / 2) & 1));
           tmem_fence_after();
-#pragma unroll 1
-          for (int g = 0; g < vg; ++g) {
+#pragma unroll
+          for (int g = 0; g < VG; ++g) {
+            if (g >= vg) break;
 #pragma unroll 1
             for (int h = 0; h < RH; h += 8) {
               float o[kDaTermsP][8];
