@@ -281,7 +281,9 @@ int hisparse_read_records(const hisparse_record_format_t *format, int device, co
  * A token that sees no key gets out = 0, lse = -inf.  Rows of out and lse that belong to no request stay as they are.
  *   slot table of hisparse_resolve: page_size 1, q_start_dev = kv_len_dev = NULL (one token a request, table_width = k)
  *   paged cache: page_size records a page, the chunk's own records already written (hisparse_write_records)
- * Masked keys may hold anything, NaN and infinities included: they do not reach a token that does not see them.
+ * Masked keys may hold anything, NaN and infinities included: they do not reach a token that does not see them.  Only the keys of
+ * a chunk's own later tokens are read at all; where one is not finite, the rows of its tile that do not see it are computed
+ * again one by one, by a warp each and key by key: right, but up to thousands of times slower.
  * Device-side lengths that do not fit the arguments set STATUS_OUT_OF_RANGE in *status_dev (may be NULL) and touch nothing
  * outside the tensors: a request whose rows leave q is skipped, a chunk longer than max_q_len is cut to it, a context
  * longer than max_kv_len or table_width pages ends there, a table entry beyond num_records is an absent page.
@@ -304,7 +306,7 @@ typedef struct {
   int64_t table_stride;
   int32_t table_width;              /* table_width * page_size at most 2^31 - 1024 */
   int32_t page_size;
-  int32_t num_requests;
+  int32_t num_requests;             /* at least 1, and so are table_width, page_size and max_q_len */
   int32_t num_heads;                /* 1 .. HISPARSE_MAX_HEADS, all sharing the request's records */
   int32_t value_dims;               /* 128, 256 or 512, at most dims */
   const void *q_dev;                /* bf16, row (token, head) of D numbers at token * q_token_stride + head * q_head_stride */
@@ -325,8 +327,10 @@ typedef struct {
 /* Device scratch that hisparse_record_attention needs for this problem (the same fields; pointers are not read, except
  * whether q_start_dev is NULL): partial results where a context is split over blocks, and the records as bf16 rows
  * (num_requests * max_kv_len * 2 dims bytes, at most 2 GB) where many rows a request read quantised records or small
- * pages.  May be 0.  Caller-owned: two calls that may overlap need one each.  The call enqueues one to three kernels and
- * allocates nothing; capturable. */
+ * pages.  Where that is more than 2 GB those rows are attended from the records as they are, at about half the rate.  May be 0.
+ * Caller-owned: two calls that may overlap need one each.  The call enqueues one to three kernels and allocates nothing;
+ * capturable.  A successor that the caller launches with programmatic stream serialization may start while they run, and has
+ * to execute griddepcontrol.wait before it reads their results or writes what they read. */
 int hisparse_record_attention_workspace_bytes(const hisparse_record_attention_t *problem, size_t *bytes);
 int hisparse_record_attention(const hisparse_record_attention_t *problem, void *workspace_dev, size_t workspace_bytes, void *stream);
 
