@@ -317,7 +317,7 @@ class _Launch:
         s = stream
         if isinstance(stream, int):
             # (0 and 1 are the legacy default stream; torch takes a number of 0 for none and makes a stream of its own)
-            s = torch.cuda.ExternalStream(stream, device=device) if stream > 1 else torch.cuda.default_stream(device)
+            s = torch.cuda.default_stream(device) if stream in (0, 1) else torch.cuda.ExternalStream(stream, device=device)
         if s.device.index != device:
             raise ValueError("stream: expected a stream of cuda:%d" % device)
         self.ptr, self._ctx = s.cuda_stream, torch.cuda.stream(s)
